@@ -105,7 +105,7 @@ def rmsnorm_bwd(dy, z, weight, rstd, dsum):
 
 # ---- gated projections ------------------------------------------------------------------------------------------------------
 
-_erf = np.vectorize(math.erf, otypes=[np.float64])
+_erfc = np.vectorize(math.erfc, otypes=[np.float64])
 
 
 def activation(g, name):
@@ -114,7 +114,7 @@ def activation(g, name):
         with np.errstate(over="ignore"):
             p = 1.0 / (1.0 + np.exp(-g))
         return g * p, p + g * p * (1.0 - p)
-    cdf = 0.5 * (1.0 + _erf(g / math.sqrt(2.0)))
+    cdf = 0.5 * _erfc(-g / math.sqrt(2.0))   # 1 + erf has no digits left where g is far below zero
     return g * cdf, cdf + g * np.exp(-g * g / 2.0) / math.sqrt(2.0 * math.pi)
 
 
