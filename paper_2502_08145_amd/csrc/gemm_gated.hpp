@@ -12,10 +12,21 @@ namespace axonn {
 // ---- activations -------------------------------------------------------------------------------------------------------------
 enum { kSilu = 0, kGelu = 1 };
 
-// act(g), and its derivative.  The exponential of the fast path is off by a few units of 2^-24, against the 2^-9 of the result's rounding.
+// act(g), and its derivative.  The fast path's exponential rounds its argument times log2(e), so that it is off by up to |g| 2^-23 of itself (the density's
+// by g^2 2^-23), 2^-15 at the ends of the range, against the 2^-9 of the result's rounding.
+//
+// GELU's distribution function below -|g| is density(g) P(t) with t = 1 / (1 + 0.36 |g|), which has its digits however small the value is; 1 + erf has none
+// left there (at -5.5 half of the value, at -6 all of it).  P, a polynomial without constant term, was fitted to exp(g^2 / 2) times the function over
+// 0 <= |g| <= 14 for the least relative error, 2^-20.  The exponential is the slope's too.  (Gradients of 2048 x 8192: 29.9 us, with erfc 33.4,
+// with 1 + erf 30.9.)
+__device__ __forceinline__ float normal_below(float g, float exponential) {   // exponential: exp(-g^2 / 2)
+    const float t = __builtin_amdgcn_rcpf(1.f + 0.36f * fabsf(g));
+    const float tail = exponential * t * (0.14371304f + t * (0.14177249f + t * (0.13971901f + t * (0.02655006f + t * (0.18095289f + t * (-0.17976384f + t * 0.04705604f))))));
+    return g < 0.f ? tail : 1.f - tail;
+}
 __device__ __forceinline__ float activation(int act, float g) {
     if (act == kSilu) return g / (1.f + __expf(-g));
-    return g * (0.5f * (1.f + erff(g * 0.70710678f)));
+    return g * normal_below(g, __expf(-0.5f * g * g));
 }
 __device__ __forceinline__ float activation(int act, float g, float* slope) {
     if (act == kSilu) {
@@ -23,8 +34,8 @@ __device__ __forceinline__ float activation(int act, float g, float* slope) {
         *slope = p * (1.f + g * (1.f - p));
         return g * p;
     }
-    const float p = 0.5f * (1.f + erff(g * 0.70710678f));
-    *slope = p + g * (__expf(-0.5f * g * g) * 0.39894228f);
+    const float exponential = __expf(-0.5f * g * g), p = normal_below(g, exponential);
+    *slope = p + g * (exponential * 0.39894228f);
     return g * p;
 }
 
