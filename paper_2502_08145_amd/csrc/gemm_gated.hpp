@@ -366,14 +366,15 @@ __global__ __launch_bounds__(1024) void gated_rows_kernel(const uint16_t* __rest
 }
 
 // ---- what none of the others takes (D < 8, F < 16 in NN, leading dimensions of 2^24 and more) ---------------------------------------------------------------------------------------------------
-// 64 x 64 of h by 2 x 2 waves, 32 k at a time: what a thread stages of the next 32 k is on its way to registers while this one's is multiplied from LDS,
+// Blocks from `first` on, 64 x 64 of h each by 2 x 2 waves, 32 k at a time: what a thread stages of the next 32 k is on its way to registers while this one's is multiplied from LDS,
 // where both operands lie K-contiguous in rows of 32 k and 16 bytes more (sixteen rows then start in different banks).
 template <bool B_KC>
-__global__ __launch_bounds__(256) void gated_any_kernel(const uint16_t* __restrict__ X, const uint16_t* __restrict__ W, int64_t M, int64_t D, int64_t blocks_n, GatedOut out) {
+__global__ __launch_bounds__(256) void gated_any_kernel(const uint16_t* __restrict__ X, const uint16_t* __restrict__ W, int64_t M, int64_t D, int64_t first, int64_t blocks_n,
+                                                        GatedOut out) {
     constexpr int LD = 40;   // bf16 of an LDS row
     __shared__ __attribute__((aligned(16))) uint16_t panel[3][64][LD];   // x, Wg, Wu
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, wm = wave >> 1, wn = wave & 1, r16 = lane & 15, quad = lane >> 4;
-    const int64_t m0 = (int64_t)(blockIdx.x / blocks_n) * 64, n0 = (int64_t)(blockIdx.x % blocks_n) * 64, F = out.F;
+    const int64_t block = first + blockIdx.x, m0 = block / blocks_n * 64, n0 = block % blocks_n * 64, F = out.F;
     const int row = t >> 2, chunk = 8 * (t & 3);      // of a K-contiguous panel
     const int k_row = t >> 3, n_chunk = 8 * (t & 7);  // of W as [D, 2F]
     const u32x4 none = {0u, 0u, 0u, 0u};

@@ -92,6 +92,8 @@ struct GatedChoice {
     }
 };
 
+constexpr int64_t kMaxWorkgroups = (int64_t)1 << 22;   // of a launch: times 512 threads below 2^32
+
 // The kernel with the shortest modelled time; the models are those of a product with an output of M x 2F, which takes as long, but for NN tiles
 // whose halves are not whole lines (1.1 and 1.03, by the choices on 30 products of 1 to 299 rows).
 static GatedChoice gated_choose(int64_t M, int64_t F, int64_t D, bool nt) {
@@ -100,7 +102,7 @@ static GatedChoice gated_choose(int64_t M, int64_t F, int64_t D, bool nt) {
     GatedChoice best;
     if (D % 8 == 0 && F % 8 == 0 && D > 64 && D < (1 << 23) && F < (1 << 22) && (!nt || (F + 256) * D * 2 < ((int64_t)1 << 32))) {
         for (const GatedTile& t : kGatedTiles) {
-            if (M < t.bm || 2 * F < t.bn) continue;
+            if (M < t.bm || 2 * F < t.bn || ((M + t.bm - 1) / t.bm) * ((F + t.bn / 2 - 1) / (t.bn / 2)) >= kMaxWorkgroups) continue;
             if (t.groups) {
                 best.consider((nt || t.bn > 64 ? 1.0 : 1.1) * group_us(t.bm, t.bn, t.groups, layout, M, 2 * F, D, D, ldw, 2 * F), &t, nullptr, 0);
             } else {
@@ -156,7 +158,6 @@ static int gated_forward(int64_t M, int64_t F, int64_t D, int layout, const uint
     if (how.tile) {
         const GatedTile& t = *how.tile;
         const int64_t tiles_m = (M + t.bm - 1) / t.bm, tiles_n = (F + t.bn / 2 - 1) / (t.bn / 2);
-        if (tiles_m * tiles_n >= (1 << 22)) return AXONN_ERR_UNSUPPORTED;
         const int k_tail = (int)(D % 64);
         hipLaunchKernelGGL(t.fn[nt][k_tail != 0], dim3((unsigned)(tiles_m * tiles_n)), dim3(t.threads), t.lds_bytes, s, X, W, (int)(D - k_tail + (k_tail ? 64 : 0)), (int)D,
                            (int)(nt ? D : 2 * F), TileGrid{(int)tiles_m, (int)tiles_n, (int)(M - t.bm), (int)(F - t.bn / 2), k_tail}, (int)std::min<int64_t>(tiles_m, 8), out);
@@ -167,8 +168,9 @@ static int gated_forward(int64_t M, int64_t F, int64_t D, int layout, const uint
                            (int)std::min<int64_t>(tiles_m, 8), out);
     } else {
         const int64_t blocks_n = (F + 63) / 64, blocks = blocks_n * ((M + 63) / 64);
-        if (blocks >= (1 << 23)) return AXONN_ERR_UNSUPPORTED;
-        hipLaunchKernelGGL((nt ? gated_any_kernel<true> : gated_any_kernel<false>), dim3((unsigned)blocks), dim3(256), 0, s, X, W, M, D, blocks_n, out);
+        for (int64_t first = 0; first < blocks; first += kMaxWorkgroups)
+            hipLaunchKernelGGL((nt ? gated_any_kernel<true> : gated_any_kernel<false>), dim3((unsigned)std::min(blocks - first, kMaxWorkgroups)), dim3(256), 0, s, X, W, M, D, first,
+                               blocks_n, out);
     }
     return hipGetLastError() == hipSuccess ? AXONN_OK : AXONN_ERR_LAUNCH;
 }

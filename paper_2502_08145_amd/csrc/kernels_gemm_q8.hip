@@ -42,21 +42,31 @@ __global__ __launch_bounds__(256) void q8_zero_kernel(uint16_t* c, int64_t count
 }  // namespace rows
 using namespace rows;
 
-// The tile with the shortest modelled time: whole rounds, and what is left of one; nullptr: the kernel for few rows.  Both are bound by reading b where there
+constexpr int64_t kMaxWorkgroups = (int64_t)1 << 22;   // of a launch: times 512 threads below 2^32
+struct Q8Choice {
+    const Q8Variant* tile = nullptr;
+    bool few_rows = false;   // neither: no kernel takes that many workgroups
+};
+// The tile with the shortest modelled time: whole rounds, and what is left of one; or the kernel for few rows.  Both are bound by reading b where there
 // are few rows of a: tiles at 6.7 MB/us (33 x 16384 x 4096 12.5 us), the other kernel at 5.6 to 2.9 as a gets more rows (4, 16 and 32 rows: 14.4, 17.9 and
 // 25.8 us), but over few rows of b its workgroups share K where a tile takes it all (32 x 4096 x 4096 9.0 us and 9.8, 8 x 4096 x 16384 18 and 34).
-static const Q8Variant* q8_choose(int64_t M, int64_t N, int64_t steps) {
+static Q8Choice q8_choose(int64_t M, int64_t N, int64_t steps) {
     constexpr int64_t kUnits = 256;
     const double b_bytes = (double)N * (double)steps * 128.0;
-    const Q8Variant* best = nullptr;
-    double best_us = M <= 32 ? 2.5 + b_bytes / (M <= 4 ? 5.6e6 : M <= 16 ? 4.4e6 : 2.9e6) : 0.0;
+    Q8Choice best;
+    double best_us = 0.0;
+    if (M <= 32 && (N + 15) / 16 < kMaxWorkgroups) {
+        best.few_rows = true;
+        best_us = 2.5 + b_bytes / (M <= 4 ? 5.6e6 : M <= 16 ? 4.4e6 : 2.9e6);
+    }
     for (const Q8Variant& v : kQ8Tiles) {
         const int64_t tiles = ((M + v.bm - 1) / v.bm) * ((N + v.bn - 1) / v.bn), round = kUnits * v.per_unit, rest = tiles % round;
+        if (tiles >= kMaxWorkgroups) continue;
         double us = (double)(tiles / round) * ((double)steps * v.step + v.fixed);
         if (rest) us += (double)steps * (rest > kUnits ? v.step : v.step_alone) + v.fixed;
         us = std::max(us, 2.5 + b_bytes / 6.7e6);
-        if ((!best && M > 32) || us < best_us) {
-            best = &v;
+        if ((!best.tile && !best.few_rows) || us < best_us) {
+            best = Q8Choice{&v, false};
             best_us = us;
         }
     }
@@ -83,18 +93,17 @@ extern "C" int axonn_q8_linear(int64_t M, int64_t N, int64_t K, const void* a, c
         hipLaunchKernelGGL(q8_zero_kernel, dim3((unsigned)std::min<int64_t>((M * N + 255) / 256, 1 << 16)), dim3(256), 0, s, (uint16_t*)c, M * N);
         return hipGetLastError() == hipSuccess ? AXONN_OK : AXONN_ERR_LAUNCH;
     }
-    const Q8Variant* const tile = q8_choose(M, N, row_bytes / 128);
-    if (!tile) {   // at most 32 rows
-        const int64_t blocks_n = (N + 15) / 16;
-        if (blocks_n >= (1 << 22)) return AXONN_ERR_UNSUPPORTED;
-        hipLaunchKernelGGL((M <= 16 ? q8_rows_kernel<1> : q8_rows_kernel<2>), dim3((unsigned)blocks_n), dim3(512), 0, s, A, B, (uint16_t*)c, row_bytes);
+    const Q8Choice how = q8_choose(M, N, row_bytes / 128);
+    if (how.few_rows) {   // at most 32
+        hipLaunchKernelGGL((M <= 16 ? q8_rows_kernel<1> : q8_rows_kernel<2>), dim3((unsigned)((N + 15) / 16)), dim3(512), 0, s, A, B, (uint16_t*)c, row_bytes);
+    } else if (!how.tile) {
+        return AXONN_ERR_UNSUPPORTED;
     } else {
         int dev = 0;
         if (hipGetDevice(&dev) == hipSuccess && dev >= 0 && dev < kMaxDevices) std::call_once(g_q8_once[dev], q8_raise_lds_limits);
         else q8_raise_lds_limits();
-        const Q8Variant& v = *tile;
+        const Q8Variant& v = *how.tile;
         const int64_t tiles_m = (M + v.bm - 1) / v.bm, tiles_n = (N + v.bn - 1) / v.bn;
-        if (tiles_m * tiles_n >= (1 << 22)) return AXONN_ERR_UNSUPPORTED;
         hipLaunchKernelGGL(v.fn, dim3((unsigned)(tiles_m * tiles_n)), dim3(v.threads), v.lds_bytes, s, A, B, (uint16_t*)c, row_bytes, (int)tiles_m, (int)tiles_n,
                            (int)std::min<int64_t>(tiles_m, 8));
     }
