@@ -778,11 +778,13 @@ static void raise_lds_limits() {
     edge_kernel_raise_lds_limit();
     wavek_raise_lds_limit();
     group_raise_lds_limit();
+    q8_raise_lds_limit();
+    gated_raise_lds_limit();
     (void)hipGetLastError();
 }
 
 // once per device, the first time a kernel that needs it is about to be launched there
-static void raise_lds_limits_once() {
+void raise_lds_limits_once() {
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) {
         (void)hipGetLastError();

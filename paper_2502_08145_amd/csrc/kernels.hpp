@@ -78,4 +78,11 @@ void wavek_raise_lds_limit();
 void wavek_launch(const WaveKChoice& c, int layout, hipStream_t s, const uint16_t* A, const uint16_t* B, uint16_t* C,
                   int64_t m, int64_t n, int64_t K, int64_t lda, int64_t ldb, int64_t ldc);
 
+// the kernels around a feed-forward block's products
+void q8_raise_lds_limit();
+void gated_raise_lds_limit();
+
+// The LDS limits of all of these kernels, once per device, before the first of them is launched there (axonn_linear.hip).
+void raise_lds_limits_once();
+
 }  // namespace axonn

@@ -3,7 +3,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <mutex>
 
 #include "../../include/axonn_linear.h"
 #include "gemm_gated.hpp"
@@ -63,10 +62,7 @@ static int gated_wavek_waves(const GatedWaveK& t, bool nt) {
     return waves;
 }
 
-constexpr int kMaxDevices = 64;
-static std::once_flag g_gated_once[kMaxDevices];
-
-static void gated_raise_lds_limits() {
+void gated_raise_lds_limit() {
     for (const GatedTile& t : kGatedTiles)
         for (const auto& layout : t.fn)
             for (const gated_tile_t fn : layout)
@@ -75,7 +71,6 @@ static void gated_raise_lds_limits() {
         for (const gated_wavek_t fn : {t.fn[0], t.fn[1], t.past})
             if (fn) (void)hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize,
                                               gated_wavek_lds(t, gated_wavek_waves(t, fn != t.fn[0]), fn != t.fn[0]));
-    (void)hipGetLastError();
 }
 
 struct GatedChoice {
@@ -150,11 +145,7 @@ static int gated_forward(int64_t M, int64_t F, int64_t D, int layout, const uint
         return hipGetLastError() == hipSuccess ? AXONN_OK : AXONN_ERR_LAUNCH;
     }
     const GatedChoice how = gated_choose(M, F, D, nt);
-    if (how.tile || how.wavek) {
-        int dev = 0;
-        if (hipGetDevice(&dev) == hipSuccess && dev >= 0 && dev < kMaxDevices) std::call_once(g_gated_once[dev], gated_raise_lds_limits);
-        else gated_raise_lds_limits();
-    }
+    if (how.tile || how.wavek) raise_lds_limits_once();
     if (how.tile) {
         const GatedTile& t = *how.tile;
         const int64_t tiles_m = (M + t.bm - 1) / t.bm, tiles_n = (F + t.bn / 2 - 1) / (t.bn / 2);

@@ -2,10 +2,10 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <mutex>
 
 #include "../../include/axonn_linear.h"
 #include "gemm_q8.hpp"
+#include "kernels.hpp"
 
 namespace axonn {
 
@@ -27,12 +27,8 @@ static Q8Variant q8_variant(double step, double step_alone, double fixed) {
 static const Q8Variant kQ8Tiles[] = {q8_variant<256, 256, 2, 4, 2, true>(1.30, 1.15, 6.0), q8_variant<256, 128, 4, 2, 2, true>(0.93, 0.75, 3.0),
                                      q8_variant<128, 128, 2, 4, 2, true>(0.98, 0.57, 3.0), q8_variant<64, 64, 2, 2, 4, false>(0.40, 0.25, 2.0)};
 
-constexpr int kMaxDevices = 64;
-static std::once_flag g_q8_once[kMaxDevices];
-
-static void q8_raise_lds_limits() {
+void q8_raise_lds_limit() {
     for (const Q8Variant& v : kQ8Tiles) (void)hipFuncSetAttribute(reinterpret_cast<const void*>(v.fn), hipFuncAttributeMaxDynamicSharedMemorySize, v.lds_bytes);
-    (void)hipGetLastError();
 }
 
 namespace rows {
@@ -99,9 +95,7 @@ extern "C" int axonn_q8_linear(int64_t M, int64_t N, int64_t K, const void* a, c
     } else if (!how.tile) {
         return AXONN_ERR_UNSUPPORTED;
     } else {
-        int dev = 0;
-        if (hipGetDevice(&dev) == hipSuccess && dev >= 0 && dev < kMaxDevices) std::call_once(g_q8_once[dev], q8_raise_lds_limits);
-        else q8_raise_lds_limits();
+        raise_lds_limits_once();
         const Q8Variant& v = *how.tile;
         const int64_t tiles_m = (M + v.bm - 1) / v.bm, tiles_n = (N + v.bn - 1) / v.bn;
         hipLaunchKernelGGL(v.fn, dim3((unsigned)(tiles_m * tiles_n)), dim3(v.threads), v.lds_bytes, s, A, B, (uint16_t*)c, row_bytes, (int)tiles_m, (int)tiles_n,

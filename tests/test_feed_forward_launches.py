@@ -56,3 +56,33 @@ def test_the_general_kernel_in_several_launches_covers_its_output_once(run, M, F
     answer, = run([gated_fwd(M, F, D, layout)])
     assert len(answer.launches) > 1 and all("gated_any_kernel" in x.kernel for x in answer.launches)
     assert sum(x.workgroups for x in answer.launches) == -(-M // 64) * -(-F // 64)
+
+
+FIRST_CALLS = [q8_linear(8192, 8192, 256), q8_linear(2048, 4096, 16384), q8_linear(1000, 1000, 256), q8_linear(64, 64, 256), gated_fwd(2048, 8192, 4096, NN), gated_fwd(2048, 8192, 4096, NT),
+               gated_fwd(299, 2088, 1608, NN), gated_fwd(300, 2048, 128, NT), gated_fwd(16, 8192, 4096, NT), gated_fwd(40, 501, 777, NN),
+               ("axonn_linear_fwd", [2048, 4096, 4096, NN, A, A, A, 1, 0])]
+
+
+@pytest.mark.parametrize("call", FIRST_CALLS)
+def test_lds_limits_are_raised_by_the_set_up_or_by_the_first_call(run, call):
+    init, first = run([("axonn_linear_init", []), call])
+    assert init.status == B.AXONN_OK and first.status == B.AXONN_OK and first.launches
+    assert not first.limits, "the set-up left these to the call"
+    raised = dict(init.limits)
+    for x in first.launches:
+        assert x.lds <= 64 * 1024 or raised[x.kernel] >= x.lds, x
+    first, second = run([call, call])
+    raised = dict(first.limits)
+    assert not second.limits and first.launches == second.launches
+    for x in first.launches:
+        assert x.lds <= 64 * 1024 or raised[x.kernel] >= x.lds, x
+
+
+def test_no_dynamic_lds_is_used_without_its_limit(run):
+    """Over many sizes: every launch stays within what its kernel's limit was raised to."""
+    sizes = list(itertools.product([1, 5, 16, 17, 40, 64, 130, 300, 520, 2048], [16, 72, 200, 501, 2048, 4099, 8192], [64, 136, 777, 4096]))
+    answers = run([("axonn_linear_init", [])] + [q8_linear(*s) for s in sizes] + [gated_fwd(*s, layout) for s in sizes for layout in (NN, NT)])
+    raised = dict(answers[0].limits)
+    for answer in answers[1:]:
+        for x in answer.launches:
+            assert x.lds <= 64 * 1024 or raised.get(x.kernel, 0) >= x.lds, x
