@@ -26,6 +26,11 @@ void write(const char* what, const void* fn, uint64_t workgroups, uint64_t threa
 extern "C" {
 const char* host_runtime_log() { return g_log.c_str(); }
 void host_runtime_clear() { g_log.clear(); }
+const char* host_runtime_kernels() {
+    g_log.clear();
+    for (const auto& [fn, name] : g_names) g_log += name + '\n';
+    return g_log.c_str();
+}
 
 void** __hipRegisterFatBinary(const void*) {
     static void* module;

@@ -12,7 +12,7 @@ import sys
 from paper_2502_08145_amd import build
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-Launch = collections.namedtuple("Launch", "kernel workgroups threads lds")
+Launch = collections.namedtuple("Launch", "kernel workgroups threads lds")   # kernel: its mangled name
 Answer = collections.namedtuple("Answer", "status launches limits")   # limits: (kernel, bytes of LDS)
 
 _CHILD = """
@@ -46,3 +46,16 @@ def run(so, calls):
                 limits.append((kernel, int(lds)))
         answers.append(Answer(status, launches, limits))
     return answers
+
+
+def readable(kernels):
+    """{mangled name: name with its template arguments}"""
+    kernels = sorted(set(kernels))
+    out = subprocess.run(["c++filt"], input="\n".join(kernels), capture_output=True, text=True, check=True).stdout.splitlines()
+    return {k: line.split("(")[0].replace("void ", "").replace("axonn::", "") for k, line in zip(kernels, out)}
+
+
+def kernels_of_the_library(so):
+    """The mangled names of all kernels, as the library registers them"""
+    code = "import ctypes, sys; f = ctypes.CDLL(sys.argv[1], ctypes.RTLD_GLOBAL); ctypes.CDLL(sys.argv[2]); f.host_runtime_kernels.restype = ctypes.c_char_p; print(f.host_runtime_kernels().decode())"
+    return subprocess.run([sys.executable, "-c", code, so, build.LIB], capture_output=True, text=True, check=True, timeout=100).stdout.split()
