@@ -572,7 +572,7 @@ def _memory(t):
     """(address, bytes) of a contiguous CUDA tensor of any type; (0, 0) for None."""
     if t is None:
         return 0, 0
-    if not t.is_cuda or not t.is_contiguous():
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
         raise TypeError("expected a contiguous CUDA tensor")
     return t.data_ptr(), t.numel() * t.element_size()
 

@@ -86,3 +86,11 @@ def test_no_dynamic_lds_is_used_without_its_limit(run):
     for answer in answers[1:]:
         for x in answer.launches:
             assert x.lds <= 64 * 1024 or raised.get(x.kernel, 0) >= x.lds, x
+
+
+def test_scratch_memory_is_a_tensor():
+    """An address has no size: it is refused as any other that is no tensor."""
+    with pytest.raises(TypeError):
+        B.axonn_rmsnorm_bwd(8, 8, A, A, A, A, None, A, A, A, stream=0)
+    with pytest.raises(TypeError):
+        B.axonn_gated_bwd_q8(8, 8, 8, "NN", "silu", A, A, A, A, A, A, A, A, A, A, A, stream=0)
