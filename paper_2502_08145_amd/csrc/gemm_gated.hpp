@@ -49,8 +49,8 @@ struct GatedOut {
 // ---- tiles: the bf16 tile kernels with another order of b's columns ------------------------------------------------------------------
 // Of the TN columns of b that a wave multiplies the first half comes from Wg and the other half, the same columns, from Wu; the order is made where the
 // direct loads fetch, and everything between them and the sums is the tile kernels' own.  A tile of BM x BN gives BM x BN/2 of h.
-// Bound by what bounds the product of the same sizes, whose time it takes: 2048 x 8192 x 4096 NN with the sums kept 220 us, 1250 TFLOP/s, at the board's power limit;
-// 299 x 2088 x 1608 13.4 us, a chain of 26 steps on 165 of the 256 units.
+// Bound by what bounds the product of the same sizes, whose time it takes: 2048 x 8192 x 4096 NN with the sums kept 218 us, 1260 TFLOP/s, at the board's power limit;
+// 299 x 2088 x 1608 12.8 us, a chain of 26 steps on 165 of the 256 units.
 template <int BN, int TN>
 struct GatedKind {
     static constexpr bool kOwn = true;
@@ -301,7 +301,7 @@ __global__ __launch_bounds__(64 * WaveKCfg::max_waves(MI, 2 * NB)) void gated_wa
 // k 8 (lane / 4) .. of row lane % 4, are what it gives to two products of 16 independent blocks, 4 x 4 x 4 each, and x's rows are loaded the same way.
 // So no value goes through LDS, no lane waits for another, and the vector unit has no arithmetic to do; the 16 blocks' sums are added up once, behind
 // the last k, in a fixed order.
-// Bound by the way from memory: 1 x 8192 x 4096 23.2 us, 5.8 TB/s (the wave-K kernel 30.1), 1 x 13824 x 5120 44.1 (49.2).  Only D of multiples of 8: with rows at
+// Bound by the way from memory: 1 x 8192 x 4096 23.2 us, 5.8 TB/s (the wave-K kernel 30.1), 1 x 13824 x 5120 43.5 (49.2), each call with a W that no cache holds.  Only D of multiples of 8: with rows at
 // any address the pieces cross lines, and 4 x 4096 x 1001 took 10 us where the wave-K kernel takes 7.  Nor more rows: every workgroup loads all of x, and
 // 8 x 8192 x 4096 took 33.
 // Requires D % 8 == 0, M <= 4.
@@ -440,7 +440,9 @@ __global__ __launch_bounds__(256) void gated_any_kernel(const uint16_t* __restri
 }
 
 // ---- the gradients of the activation and the product ------------------------------------------------------------------------------
-// dg = dh u act'(g), du = dh act(g), side by side as [M, 2F], and h again, eight columns a thread; one rounding each.  Q8: g and u come from the 8-bit
+// dg = dh u act'(g), du = dh act(g), side by side as [M, 2F], and h again, eight columns a thread.  dg and du are rounded to bf16 because they are operands of
+// two products on the bf16 matrix unit, whose gradients are then 0.0023 of their norm off (0.0017 with their own rounding alone); in fp32 they would be twice
+// the bytes and a sixteenth of the unit's rate.  Q8: g and u come from the 8-bit
 // format, rows of 2F.  RAGGED: F is no multiple of 8 (u's pieces then start at any byte).  Bound by memory: 10 or 8 bytes an element and 2 for h;
 // 2048 x 4096 18 to 20 us (101 MB), from 8 bits 17 to 18 (84 MB).
 // Q8: workgroups from slope_groups on restore the other matrix that was kept, which the products want (a launch of its own took 3.5 us where all of it is small).

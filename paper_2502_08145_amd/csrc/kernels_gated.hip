@@ -37,8 +37,9 @@ struct GatedWaveK {
     gated_wavek_t fn[2];
     gated_wavek_t past;   // NT, W past the caches
 };
-// A W of 64 MB and more, read once, goes past the caches: with a few such layers none of it is still there at the next call.  16 x 8192 x 4096 30.2 -> 25.7 us,
-// 1 x 8192 x 4096 26.2 -> 23.2; where it would have been there, 21.2 -> 22.0.  32 MB: 8.6 and 8.7, with all of it in the caches 7.2 and 7.3.  (NN gains nothing.)
+// A W of 64 MB and more, read once, goes past the caches: with a few such layers none of it is still there at the next call.  Eight layers' W in turn:
+// 16 x 8192 x 4096 30.2 -> 26.7 us, 1 x 8192 x 4096 26.2 -> 23.2, 16 x 4096 x 4096 14.7 -> 13.2; one W again and again, which a program of one layer would
+// do, 21.0 -> 25.9, 21.1 -> 22.4, 12.1 -> 12.9.  32 MB: 8.6 and 8.7, with all of it in the caches 7.2 and 7.3.  (NN gains nothing.)
 static bool gated_past(int64_t F, int64_t D) { return 2 * F * D >= (int64_t)1 << 25; }
 // NN: the blocks of either half are 32 bytes of a k-row each.  One doubles the workgroups where there are few (1 x 2048 x 4096 18.2 us with two, 16.0 with one)
 // and costs the way from memory where there are enough (16 x 8192 x 4096 35 and 52, 48 x 4096 x 4096 19 and 26): up to F = 4096 and 32 rows.  Four are
